@@ -551,7 +551,7 @@ int ipk_linear_destroy(ipk_linear_t* h);
  * IPK_MAX_BATCH] and max_T in [1, IPK_MAX_T] size the workspace.
  * Ranges: |gn_mult| < 2^24, |gn_bias| < 2^56, gn_shift in [1, 62], eps >= 1 (in 2^-16 of
  * z's squared steps).  With swish != 0: 0 <= sw_qc < 2^20, |sw_q1| < 2^45, 0 <= m_sw < 2^23,
- * shift_sw in [1, 62], and |Swish(h)| m_sw + 2^(shift_sw - 1) < 2^62 for every int16 h
+ * shift_sw in [1, 62], and |Swish(h)| m_sw + 2^(shift_sw - 1) < 2^63 for every int16 h
  * (IPK_ERR_UNSUPPORTED otherwise); with swish = 0 they are not read.
  */
 typedef struct ipk_groupnorm_desc {

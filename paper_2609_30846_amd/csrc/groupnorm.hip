@@ -132,6 +132,7 @@ __device__ __forceinline__ void coefficients(const Stats& s, int mult, int64_t b
 // Eq. 12's Swish of an int16 value and its requantization: -(|h| L + h q1) is -h (t^2 + 2 q1) for
 // h >= 0 and h t^2 below, t = qc - min(|h|, qc): the median of qc - h, qc + h and 0.
 //  FAST: |h m_sw| and t^2 + 2 |q1| stay below 2^31 and shift_sw >= 32: one 64-bit multiply-add
+//  otherwise products of 64 bits, exact as the accepted constants keep h w m_sw + 2^(shift_sw-1) below 2^63
 template <bool FAST>
 __device__ __forceinline__ int swish(int h, const GroupNorm& g) {
   const int a = g.sw_qc - h, b = g.sw_qc + h;

@@ -1322,8 +1322,8 @@ static int validate_groupnorm(const ipk_groupnorm_desc* D) {
     const __int128 av = v < 0 ? -v : v;
     __int128 q = -(av * poly_l128(av, D->sw_qc, D->sw_q1) + (__int128)v * D->sw_q1);
     if (q < 0) q = -q;
-    if (q * D->m_sw + ((__int128)1 << (D->shift_sw - 1)) >= ((__int128)1 << 62))
-      return fail(IPK_ERR_UNSUPPORTED, "Swish of the int16 value %d times m_sw reaches 2^62", v);
+    if (q * D->m_sw + ((__int128)1 << (D->shift_sw - 1)) >= ((__int128)1 << 63))
+      return fail(IPK_ERR_UNSUPPORTED, "Swish of the int16 value %d times m_sw reaches 2^63", v);
   }
   return IPK_OK;
 }
