@@ -171,7 +171,7 @@ def _norm_constants(g, case):
     su = UNIT16 / 2
     sw_qc, sw_q1 = math.floor(SWISH_C / su), math.floor(1.0 / (SWISH_A * su * su))
     ratio = UNIT16 / (2.0 * -sw_q1) / GRID[case["out"]]
-    shift_sw = 15 - math.floor(math.log2(ratio))  # m_sw of 16 bits: |Swish| m_sw stays below 2^62
+    shift_sw = 16 - math.floor(math.log2(ratio))
     return {"mult": mult, "bias": bias, "shift": shift, "eps": eps, "sw_qc": sw_qc, "sw_q1": sw_q1,
             "m_sw": int(round(ratio * 2.0 ** shift_sw)), "shift_sw": shift_sw}
 
