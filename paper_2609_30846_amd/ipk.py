@@ -4,6 +4,10 @@ Every step of the block runs in the HIP kernels of ``libipk.so``.  There is no
 fallback: ``load()`` raises if the library is not built, and every entry point
 raises ``IpkError`` when the library returns a non-zero status.  Device buffers
 are torch tensors on the current HIP device; streams are torch streams.
+
+A call runs on the current stream, or on the ``stream`` it is given.  Then what it reads has to be
+ready there (``stream.wait_stream``), and other streams wait for it before they read what it
+wrote; tensors may be dropped as soon as the call has returned, as without a stream.
 """
 
 from __future__ import annotations
@@ -278,6 +282,40 @@ def _stream_ptr(stream, index: Optional[int] = None) -> Optional[int]:
     return int(stream.cuda_stream)
 
 
+def _side(stream, index: Optional[int]):
+    """``stream`` where it is not the current stream of device ``index`` (the current device's), None otherwise
+    (and without a stream).
+
+    torch hands out memory by streams: a block goes back to the stream that it was allocated for when its tensor
+    is dropped, and that stream's next tensor may take it without waiting for any other.  So a call on
+    another stream allocates what it returns there (_new), and tells the allocator which tensors
+    it uses (_used): they may be dropped as soon as the call returns.  Both are the caller's
+    where the raw ipk_*_run functions are called."""
+    return None if stream is None or int(stream.cuda_stream) == _stream_ptr(None, index) else stream
+
+
+def _new(side, make, *args, **kwargs):
+    """make(...)'s tensor, allocated for the stream ``side`` if there is one, on which the call writes
+    it; the caller's current stream may read it up to the moment it is dropped."""
+    if side is None:
+        return make(*args, **kwargs)
+    import torch
+
+    current = torch.cuda.current_stream()
+    with torch.cuda.stream(side):
+        t = make(*args, **kwargs)
+    t.record_stream(current)
+    return t
+
+
+def _used(side, *tensors) -> None:
+    """The work that ``side`` now has uses ``tensors`` (None: no such tensor)."""
+    if side is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(side)
+
+
 def ipk_relpos_attn_create(desc: Desc) -> int:
     h = _vp()
     _check(load().ipk_relpos_attn_create(C.byref(desc), C.byref(h)))
@@ -413,9 +451,11 @@ class RelPosAttn:
         import torch
 
         B, T, lengths = self._check_run(x, pos_table, lengths, y)
+        side = _side(stream, self._dev.index)
         if y is None:
-            y = torch.empty_like(x)
+            y = _new(side, torch.empty_like, x)
         ipk_relpos_attn_run(self.handle, x, pos_table, lengths, B, T, y, stream)
+        _used(side, x, pos_table, y)
         return y
 
     def run_noalloc(self, x, pos_table, lengths=None, y=None, stream=None):
@@ -425,6 +465,7 @@ class RelPosAttn:
             raise ValueError("run_noalloc writes into the caller's y")
         B, T, lengths = self._check_run(x, pos_table, lengths, y)
         ipk_relpos_attn_run_noalloc(self.handle, x, pos_table, lengths, B, T, y, stream)
+        _used(_side(stream, self._dev.index), x, pos_table, y)
         return y
 
     def repeat_core(self, count: int, stream=None):
@@ -440,6 +481,7 @@ class RelPosAttn:
         T_table = (pos_table.shape[0] + 1) // 2
         _tensor(pos_table, "pos_table", (2 * T_table - 1, self.d_model), self._dev)
         ipk_relpos_attn_cache_positions(self.handle, pos_table, T_table, stream)
+        _used(_side(stream, self._dev.index), pos_table)
 
     def set_residual(self, ln_mult, ln_bias, ln_shift: int, m_z: int, m_y: int, shift_r: int):
         """LayerNorm and residual constants of the MHSA module (host arrays)."""
@@ -457,15 +499,17 @@ class RelPosAttn:
         import torch
 
         B, T, lengths = self._check_run(z1, pos_table, lengths, z2)
+        side = _side(stream, self._dev.index)
         if z2 is None:
-            z2 = torch.empty_like(z1)
+            z2 = _new(side, torch.empty_like, z1)
         ipk_mhsa_residual_run(self.handle, z1, pos_table, lengths, B, T, z2, stream)
+        _used(side, z1, pos_table, z2)
         return z2
 
     def intermediate(self, which: int, shape, stream=None):
         import torch
 
-        dst = torch.empty(shape, dtype=torch.int8, device=self.device)
+        dst = _new(_side(stream, self._dev.index), torch.empty, shape, dtype=torch.int8, device=self.device)
         ipk_relpos_attn_intermediate(self.handle, which, dst, stream)
         return dst
 
@@ -536,16 +580,18 @@ class FeedForward:
         _tensor(z, "z", tuple(z.shape), self._dev)
         if z_out is not None:
             _tensor(z_out, "z_out", tuple(z.shape), self._dev)
+        side = _side(stream, self._dev.index)
         if z_out is None:
-            z_out = torch.empty_like(z)
+            z_out = _new(side, torch.empty_like, z)
         ipk_ffn_run(self.handle, z, rows, z_out, stream)
+        _used(side, z, z_out)
         return z_out
 
     def intermediate(self, which: int, rows: int, stream=None):
         import torch
 
-        dst = torch.empty((rows, self.d_model if which == IPK_FFN_X else self.d_ff), dtype=torch.int8,
-                          device=self.device)
+        dst = _new(_side(stream, self._dev.index), torch.empty,
+                   (rows, self.d_model if which == IPK_FFN_X else self.d_ff), dtype=torch.int8, device=self.device)
         ipk_ffn_intermediate(self.handle, which, dst, stream)
         return dst
 
@@ -620,9 +666,11 @@ class ConvModule:
         if z_out is not None:
             _tensor(z_out, "z_out", (B, T, self.d_model), self._dev)
         lengths = _lengths(lengths, B, T)
+        side = _side(stream, self._dev.index)
         if z_out is None:
-            z_out = torch.empty_like(z)
+            z_out = _new(side, torch.empty_like, z)
         ipk_conv_run(self.handle, z, lengths, B, T, z_out, stream)
+        _used(side, z, z_out)
         return z_out
 
     def intermediate(self, which: int, B: int, T: int, stream=None):
@@ -631,7 +679,7 @@ class ConvModule:
         d = self.d_model
         shape, dt = {IPK_CONV_X: ((B, T, d), torch.int8), IPK_CONV_U: ((B, T, 2 * d), torch.int8),
                      IPK_CONV_V: ((B, T, d), torch.int16), IPK_CONV_O: ((B, T, d), torch.int8)}[which]
-        dst = torch.empty(shape, dtype=dt, device=self.device)
+        dst = _new(_side(stream, self._dev.index), torch.empty, shape, dtype=dt, device=self.device)
         ipk_conv_intermediate(self.handle, which, dst, stream)
         return dst
 
@@ -683,9 +731,11 @@ class LayerNorm:
         _tensor(z, "z", tuple(z.shape), self._dev)
         if x is not None:
             _tensor(x, "x", tuple(z.shape), self._dev)
+        side = _side(stream, self._dev.index)
         if x is None:
-            x = torch.empty_like(z)
+            x = _new(side, torch.empty_like, z)
         ipk_layernorm_run(self.handle, z, z.numel() // self.d_model, x, stream)
+        _used(side, z, x)
         return x
 
     def close(self):
@@ -730,12 +780,14 @@ def quantize_tokens(x, q=None, s=None, stream=None):
         raise ValueError(f"x is on {dev}, the current device is cuda:{index}")
     if not x.is_contiguous():
         raise ValueError("x must be contiguous")
+    side = None if stream is None else _side(stream, index)
     if q is None:
-        q = torch.empty_like(x, dtype=torch.int8)
+        q = torch.empty_like(x, dtype=torch.int8) if side is None else _new(side, torch.empty_like, x, dtype=torch.int8)
     else:
         _tensor(q, "q", shape, dev)
     if s is None:
-        s = x.new_empty(shape[:-1], dtype=torch.int32)
+        lead = shape[:-1]
+        s = x.new_empty(lead, dtype=torch.int32) if side is None else _new(side, x.new_empty, lead, dtype=torch.int32)
     else:
         _tensor(s, "s", shape[:-1], dev, torch.int32)
     # straight to the library, as these calls can be as short as their host time
@@ -743,6 +795,8 @@ def quantize_tokens(x, q=None, s=None, stream=None):
                                         shape[-1], q.data_ptr(), s.data_ptr(), _stream_ptr(stream, index))
     if status:
         _check(status)
+    if side is not None:
+        _used(side, x, q, s)
     return q, s
 
 
@@ -799,8 +853,9 @@ class Linear:
         out = (*lead, self.d_out)
         if z is not None:
             _tensor(z, "z", out, self._dev, self.dtype)
+        side = None if stream is None else _side(stream, self._index)
         if y is None:
-            y = q.new_empty(out, dtype=self.dtype)
+            y = q.new_empty(out, dtype=self.dtype) if side is None else _new(side, q.new_empty, out, dtype=self.dtype)
         else:
             _tensor(y, "y", out, self._dev, self.dtype)
         rows = s.numel()
@@ -811,6 +866,8 @@ class Linear:
                                        _stream_ptr(stream, self._index))
         if status:
             _check(status)
+        if side is not None:
+            _used(side, q, s, z, y)
         return y
 
     def close(self):
@@ -880,13 +937,17 @@ class GroupNorm:
         lengths = _lengths(lengths, B, T)
         if B > self.max_batch or T > self.max_T:
             raise ValueError(f"[B={B}][T={T}] exceeds max_batch={self.max_batch}, max_T={self.max_T}")
+        side = None if stream is None else _side(stream, self._index)
         if x is None:
-            x = torch.empty_like(z, dtype=self.out_dtype)
+            dt = self.out_dtype
+            x = torch.empty_like(z, dtype=dt) if side is None else _new(side, torch.empty_like, z, dtype=dt)
         lengths, lp = _host_lengths(lengths)
         status = load().ipk_groupnorm_run(self.handle, z.data_ptr(), lp, B, T, x.data_ptr(),
                                           _stream_ptr(stream, self._index))
         if status:
             _check(status)
+        if side is not None:
+            _used(side, z, x)
         return x
 
     def close(self):
