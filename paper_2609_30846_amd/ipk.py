@@ -214,6 +214,14 @@ def _ptr(t) -> int:
     return 0 if t is None else int(t.data_ptr())
 
 
+def _int(value, name: str, bits: int = 32) -> int:
+    """``value`` as an argument of ``bits`` bits, into which ctypes would wrap what does not fit."""
+    v = int(value)
+    if not -(1 << (bits - 1)) <= v < 1 << (bits - 1):
+        raise ValueError(f"{name}={v} does not fit {bits} bits")
+    return v
+
+
 def _device(device):
     """The torch device a handle lives on, with its index (the current one's if unnamed)."""
     import torch
@@ -757,8 +765,8 @@ def _dtype(type_code: int):
 
 
 def ipk_quantize_tokens(x, x_type: int, rows: int, d: int, q, s, stream=None) -> None:
-    _check(load().ipk_quantize_tokens(_ptr(x), int(x_type), int(rows), int(d), _ptr(q), _ptr(s),
-                                      _stream_ptr(stream)))
+    x_type, rows, d = _int(x_type, "x_type"), _int(rows, "rows", 64), _int(d, "d")
+    _check(load().ipk_quantize_tokens(_ptr(x), x_type, rows, d, _ptr(q), _ptr(s), _stream_ptr(stream)))
 
 
 def quantize_tokens(x, q=None, s=None, stream=None):
@@ -773,6 +781,8 @@ def quantize_tokens(x, q=None, s=None, stream=None):
         raise ValueError(f"x must be a torch.int16 or torch.int32 tensor, not {dt}")
     if not shape:
         raise ValueError("x must be [..., d]")
+    if shape[-1] > 65536:  # the C argument has 32 bits, into which more would wrap
+        raise ValueError(f"rows of {shape[-1]} values, more than 65536")
     if dev.type != "cuda":
         raise ValueError(f"x is on {dev}, not on a GPU")
     index = torch.cuda.current_device()
@@ -807,7 +817,8 @@ def ipk_linear_create(desc: LinearDesc) -> int:
 
 
 def ipk_linear_run(h: int, q, s, rows: int, z, y, stream=None) -> None:
-    _check(load().ipk_linear_run(h, _ptr(q), _ptr(s), int(rows), _ptr(z), _ptr(y), _stream_ptr(stream)))
+    rows = _int(rows, "rows")
+    _check(load().ipk_linear_run(h, _ptr(q), _ptr(s), rows, _ptr(z), _ptr(y), _stream_ptr(stream)))
 
 
 def ipk_linear_destroy(h: Optional[int]) -> None:
@@ -889,8 +900,9 @@ def ipk_groupnorm_create(desc: GroupNormDesc) -> int:
 
 
 def ipk_groupnorm_run(h: int, z, lengths: Optional[Sequence[int]], B: int, T: int, x, stream=None) -> None:
+    B, T = _int(B, "B"), _int(T, "T")
     lens, lp = _host_lengths(lengths)
-    _check(load().ipk_groupnorm_run(h, _ptr(z), lp, int(B), int(T), _ptr(x), _stream_ptr(stream)))
+    _check(load().ipk_groupnorm_run(h, _ptr(z), lp, B, T, _ptr(x), _stream_ptr(stream)))
 
 
 def ipk_groupnorm_destroy(h: Optional[int]) -> None:
