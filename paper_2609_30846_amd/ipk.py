@@ -222,6 +222,21 @@ def _int(value, name: str, bits: int = 32) -> int:
     return v
 
 
+def _ints(values, name: str, dtype):
+    """``values`` as a contiguous array of the integer type ``dtype``; ValueError where it does not hold one."""
+    a = np.asarray(values)
+    if a.dtype == dtype:
+        return np.ascontiguousarray(a)
+    try:
+        with np.errstate(invalid="ignore"):
+            b = np.ascontiguousarray(a.astype(dtype))
+        if np.array_equal(a, b):
+            return b
+    except OverflowError:  # Python integers
+        pass
+    raise ValueError(f"{name} holds values that are no {np.dtype(dtype).name}")
+
+
 def _device(device):
     """The torch device a handle lives on, with its index (the current one's if unnamed)."""
     import torch
@@ -834,16 +849,17 @@ class Linear:
         import torch
 
         dev = torch.device("cuda") if device is None else torch.device(device)
-        w = torch.as_tensor(np.ascontiguousarray(p.w, dtype=np.int8)).to(dev)
+        w = torch.as_tensor(_ints(p.w, "w", np.int8)).to(dev)
         if w.dim() != 2:
             raise ValueError(f"w must be [d_out][d_in], got shape {tuple(w.shape)}")
-        mult = np.ascontiguousarray(p.mult, dtype=np.int32)
-        bias = None if p.bias is None else np.ascontiguousarray(p.bias, dtype=np.int64)
+        mult = _ints(p.mult, "mult", np.int32)
+        bias = None if p.bias is None else _ints(p.bias, "bias", np.int64)
         for name, a in (("mult", mult), ("bias", bias)):
             if a is not None and a.shape != (w.shape[0],):
                 raise ValueError(f"{name} has shape {a.shape}, expected ({w.shape[0]},)")
         desc = LinearDesc(w.shape[1], w.shape[0], w.data_ptr(), mult.ctypes.data,
-                          None if bias is None else bias.ctypes.data, int(p.shift), int(p.m_z), int(p.out_type))
+                          None if bias is None else bias.ctypes.data, _int(p.shift, "shift"), _int(p.m_z, "m_z"),
+                          _int(p.out_type, "out_type"))
         with torch.cuda.device(dev):
             self.handle = ipk_linear_create(desc)
         self.device, self._dev = dev, _device(dev)
@@ -918,17 +934,18 @@ class GroupNorm:
         import torch
 
         dev = torch.device("cuda") if device is None else torch.device(device)
-        g = np.ascontiguousarray(p.gn_mult, dtype=np.int32)
-        c = np.ascontiguousarray(p.gn_bias, dtype=np.int64)
-        d = int(p.d_model)
+        g = _ints(p.gn_mult, "gn_mult", np.int32)
+        c = _ints(p.gn_bias, "gn_bias", np.int64)
+        d = _int(p.d_model, "d_model")
         for name, a in (("gn_mult", g), ("gn_bias", c)):
             if a.shape != (d,):
                 raise ValueError(f"{name} has shape {a.shape}, expected ({d},)")
-        desc = GroupNormDesc(d, int(p.n_groups), int(max_batch), int(max_T), int(p.in_type), int(p.out_type),
-                             g.ctypes.data, c.ctypes.data, int(p.gn_shift), int(p.eps), int(bool(p.swish)))
+        desc = GroupNormDesc(d, _int(p.n_groups, "n_groups"), _int(max_batch, "max_batch"), _int(max_T, "max_T"),
+                             _int(p.in_type, "in_type"), _int(p.out_type, "out_type"), g.ctypes.data, c.ctypes.data,
+                             _int(p.gn_shift, "gn_shift"), _int(p.eps, "eps"), int(bool(p.swish)))
         if p.swish:
-            for k in ("sw_qc", "sw_q1", "m_sw", "shift_sw"):
-                setattr(desc, k, int(getattr(p, k)))
+            for k, bits in (("sw_qc", 32), ("sw_q1", 64), ("m_sw", 32), ("shift_sw", 32)):
+                setattr(desc, k, _int(getattr(p, k), k, bits))
         with torch.cuda.device(dev):
             self.handle = ipk_groupnorm_create(desc)
         self.device, self._dev, self.d_model = dev, _device(dev), d
