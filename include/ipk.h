@@ -578,7 +578,7 @@ int ipk_groupnorm_create(const ipk_groupnorm_desc* desc, ipk_groupnorm_t** out);
 /* Runs it on `stream`: z DEVICE [B][T][d_model] of in_type -> x DEVICE [B][T][d_model] of
  * out_type, both 16-byte aligned; x may be z itself where the types are the same (in place), but
  * may not overlap it otherwise.  lengths as for ipk_conv_run.  Asynchronous; calls on one
- * handle share its workspace and must be ordered on one stream.
+ * handle, and replays of graphs that captured them, share its workspace and must be ordered on one stream.
  * Errors: IPK_ERR_INVALID_ARG (null handle or pointer, misalignment, overlap, B or T outside
  * the handle's limits, a length outside [1, T], another current device), IPK_ERR_HIP. */
 int ipk_groupnorm_run(ipk_groupnorm_t* h, const void* z, const int32_t* lengths, int32_t B, int32_t T, void* x,

@@ -67,7 +67,9 @@ __host__ __device__ __forceinline__ TilePos tile_at(const TileGrid& g, int i) {
 // (its first operands and the epilogue: plain, with the residual add, with the Swish, with token scales) plus
 // `per_k` per 1024 bytes of K, in microseconds fitted to launches of 16 .. 23000 tokens with
 // K = 256 .. 4096 and N = 256 .. 4096 (median error 3 %, and nine picks of ten within 5 % of
-// the fastest shape).  Large tiles re-use their operands best, small ones spread a short
+// the fastest shape, for the first three epilogues; the token scales' one column serves outputs of all
+// types, with and without residual: 23 picks of 26 within 5 %, the others 7 - 11 %, timed with outputs that
+// stayed in the caches).  Large tiles re-use their operands best, small ones spread a short
 // call over the chip: 125 tokens x 4096 -> 1024 take 7.8 us in 128 x 32 tiles and 27 us in
 // 256 x 128 ones, 23000 tokens 88 us in the latter and 170 us in the former; 2500 tokens
 // x 1024 -> 4096 are fastest in between (128 x 64, 15.9 us against 17.3 and 21.6 us).

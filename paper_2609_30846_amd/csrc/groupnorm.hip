@@ -11,15 +11,18 @@
 // products with gn_mult and A_c are taken in two parts.  z A_c + C_c is at most 2^53 plus the
 // bias in magnitude (|z - mean| <= sigma sqrt(n)), so it is exact whatever its terms' sizes.
 //
-// A value costs two to four bytes of traffic and about 16 integer instructions with the Swish (a 32 x 32
-// + 64-bit multiply-add for the normalization, another for the Swish, clamps and packing), 7 without, so
-// large calls are bound by memory and by issuing them in about equal parts, and small ones by the
-// launch and the trip to memory and back.  Every value that has been read stays in registers until the
+// A value costs two to four bytes of traffic and about 16 integer instructions with a Swish whose multiplier has up
+// to 16 bits (a 32 x 32 + 64-bit multiply-add for the normalization, another for the Swish, clamps and
+// packing), 24 with a wider one (64-bit products), 7 without, so large calls are bound by memory and by issuing
+// them (48 x 1000 x 1024: half of the SIMDs' cycles at 2.4 GHz, two thirds with a wide multiplier, with 3.5 waves a SIMD
+// resident on average of the six that 78 registers allow), and small ones by the launch and the trip
+// to memory and back.  Every value that has been read stays in registers until the
 // statistics are there:
 //  * one workgroup per utterance and group where a group's values fit its registers (per utterance and a
 //    few groups where those are smaller than two pieces of 16 bytes): one read, one write, one launch.
-//    48 x 1000 frames of 1024 int16 channels in 32 groups (500 to 1000 of them valid): 43 us, 4.0 TB/s of
-//    the bytes it cannot do without; 16 x 375: 8.7 us; 1 x 125: 5.2 us;
+//    48 x 1000 frames of 1024 int16 channels in 32 groups (500 to 1000 of them valid): 43.8 us, 4.0 TB/s of
+//    the bytes it cannot do without; 16 x 375: 8.7 us; 1 x 125: 5.2 us; with Swish multipliers of 17 bits
+//    50.8, 10.8 and 5.9 us;
 //  * otherwise two kernels (three with many groups): partial sums of tiles of 128 bytes of channels x some frames (integer
 //    sums, so their order does not matter), and the application, whose workgroups first add the
 //    partial sums of their groups while their own values are on the way.  2500 frames of int8 in 16
@@ -681,9 +684,10 @@ static hipError_t launch_norm(NormArgs& a, int B, hipStream_t st) {
   constexpr int PC = kPiece<TI>, SLC = 8 * PC;
   const int d = a.g.d, T = a.T, cg = d / a.g.groups;
   a.dv_cg = make_div((uint32_t)cg);
-  // One kernel with up to four pieces a lane, or up to sixteen where the workgroups fill the CUs: 4 x
-  // 500 x 1024 in 32 groups (4 pieces, 128 workgroups) 8.0 us against 10.4, 2 x 300 (4, 64) 6.2 against 9.0, 48 x
-  // 1000 (8, 1536) 43 against 51; but 1 x 400 in 8 groups (16, 8) 13.2 against 7.9.  With several groups a workgroup,
+  // One kernel with up to four pieces a lane, or up to sixteen where the workgroups fill the CUs (times with
+  // multipliers of the Swish of up to 16 bits): 4 x 500 x 1024 in 32 groups (4 pieces, 128 workgroups) 8.0 us against
+  // 10.4, 2 x 300 (4, 64) 6.2 against 9.0, 48 x 1000 (8, 1536) 43 against 51; but 1 x 400 in 8 groups (16, 8) 13.2 against
+  // 7.9.  With several groups a workgroup,
   // where it takes the place of three launches (calls / kernels alone): up to four, or eight for int16 or
   // where the CUs are filled, beyond which more registers a lane would spill.  1 x 25 x 512 int16 in 64 groups (1 piece)
   // 6.7 / 4.3 us against 12.5 / 8.1, 1 x 256 x 256 int8 in 64 (4) 10.5 / 10.1 against 12.5 / 10.1, 64 x 500 x 512 int16

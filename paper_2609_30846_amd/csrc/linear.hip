@@ -19,12 +19,14 @@
 //  * int16 and int32: a wave passes each 32 channels x 32 tokens through a piece of LDS of its own, so
 //    that eight lanes store a row's 128 bytes (four and 64 with an int16 residual).  In pieces of 16
 //    bytes a lane, 12000 tokens x 512 -> 2048 to int32 took 46.6 us instead of 29.1, 23000 x 1024 -> 4096 to int16
-//    120 instead of 111, 2500 x 1024 -> 1025 to int32 11.2 instead of 9.1; int8 takes the same time either way.
+//    120 instead of 111, 2500 x 1024 -> 1025 to int32 11.2 instead of 9.1 (all with outputs that stay in the
+//    caches, see launch_tiles); int8 takes the same time either way.
 //
 // What bounds it: with many tokens the product, at the clock the chip's power holds (23000 x 4096 -> 1024 to int8
 // with the residual 100 us, 1.93 POP/s, the library's int8 product of 8192^3 2.16); with K = 1024 its eight K steps
-// leave first operands and epilogue in sight (6000 x 1024 -> 4096 to int16 30 us, 1.68 POP/s, 49 MB of stores);
-// fewer tokens than fill the CUs once are latency.
+// leave first operands and epilogue in sight (6000 x 1024 -> 4096 to int16 30 us, 1.68 POP/s, 49 MB of stores; with
+// the residual input, as many bytes again in 64-byte runs, 45 us); fewer tokens than fill the CUs once are
+// latency (2500 x 1024 -> 1025 to int32 8.6 us: less than one wave a SIMD, eight K steps one after the other).
 #include "gemm_loop.h"
 #include "gemm_tiles.h"
 #include "ipk_internal.h"
@@ -356,12 +358,17 @@ static hipError_t launch_tiles(TokenLinearArgs& a, hipStream_t st) {
   a.tiles_total = a.grid.tiles_n * a.grid.tiles_m;
   a.per_xcd = (a.tiles_total + 7) / 8;
   const dim3 grid(8 * a.per_xcd), block(64 * NWAVE);
-  // Outputs of 16 and 32 bits leave past the caches, not to push the operands out of them, where they fill
-  // whole cache lines and are more than the caches would keep for the next call: 6000 x 1024 -> 4096 to int16 30.1
-  // us against 31.7, 23000 x 1024 -> 4096 107 against 112, 4000 x 1024 -> 1024 to int32 9.2 against 10.4; but 23000 x
-  // 256 -> 300 to int32, rows of 9.4 lines, 17.1 against 11.4, and 500 x 1024 -> 1024 to int16 with the
-  // quantization that reads them 6.6 against 6.4.  (int8 rows leave in runs of 32 bytes: 23000 x 4096 -> 1024 103
-  // against 100.)
+  // Outputs of 16 and 32 bits leave past the caches, not to push the operands out of them, where their rows
+  // are whole cache lines and they are more than the caches would keep for the next call.  Calls alone,
+  // past the caches and not, in us: 6000 x 1024 -> 4096 to int16 32.2 / 34.2, 23000 x 1024 -> 4096 113 / 120, 4200 x
+  // 1024 -> 1024 to int32 11.2 / 12.7; also where a wave's run is half a line, as in int16 with the residual input (6000 x
+  // 1024 -> 4096 44.9 / 58.5, 23000 x 4096 -> 1024 116 / 117) and in int16 from tiles of 64 and 128 channels (3000 x
+  // 1024 -> 2048 12.0 / 13.5, 17000 x 256 -> 256 6.4 / 6.9): 1 to 26 % in each of 39 calls of 8 MiB and more.  But 23000
+  // x 256 -> 300 to int32, rows of 9.4 lines, 17.1 / 11.4, and int8 rows, runs of 32 bytes, 23000 x 4096 -> 1024 103 / 100.
+  // A call that reads them next pays some of it back: with the token quantization 7 % less to 5 % more time for both
+  // (less in 28 of 39; 6000 x 1024 -> 4096 44.5 / 44.9), with a group norm 3 % less to 8 % more (more in 17 of 26;
+  // 71.4 / 68.7, and 41.1 / 41.3 for 6000 x 4096 -> 1024); below 8 MiB it is more (500 x 1024 -> 1024 to int16 and
+  // quantization 6.6 / 6.4).
   const size_t row_bytes = (size_t)a.l.N * sizeof(T);
   const bool passing = row_bytes % 128 == 0 && (uintptr_t)a.y % 128 == 0 && row_bytes * a.rows >= ((size_t)8 << 20);
   if constexpr (sizeof(T) > 1)

@@ -932,7 +932,8 @@ def ipk_groupnorm_destroy(h: Optional[int]) -> None:
 class GroupNorm:
     """Owns one group normalization handle, built from host arrays: ``p`` carries d_model,
     n_groups, in_type, out_type, gn_mult, gn_bias, gn_shift, eps, swish (a truth value) and,
-    with it, the Swish constants sw_qc, sw_q1, m_sw, shift_sw."""
+    with it, the Swish constants sw_qc, sw_q1, m_sw, shift_sw.  Calls on one object, and replays of graphs
+    that captured them, share a workspace and have to follow one another (ipk_groupnorm_run)."""
 
     def __init__(self, p, max_batch: int, max_T: int, device=None):
         import torch
